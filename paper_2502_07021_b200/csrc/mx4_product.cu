@@ -408,10 +408,12 @@ mx4_product_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_consta
             if (lane == 0) mbar_arrive(acc_empty + 8 * buf);
             if (++buf == 2) buf = 0, aph ^= 1u;
         }
-        // rows that no group has
-        const int done = row_start[A.groups], et = threadIdx.x - 32 * (2 + kScaleWarps);
-        for (int64_t r = done + (int64_t)blockIdx.x; r < A.rows; r += gridDim.x)
+        // rows that no group has: before the first one's and behind the last one's
+        const int first = row_start[0], done = row_start[A.groups], et = threadIdx.x - 32 * (2 + kScaleWarps);
+        for (int64_t k = blockIdx.x; k < first + (int64_t)(A.rows - done); k += gridDim.x) {
+            const int64_t r = k < first ? k : done + (k - first);
             for (int n = et; n < A.outs; n += 32 * kEpilogueWarps) out[r * A.ldo + n] = from_f32<OutT>(0.f);
+        }
     }
     fence_before();
     __syncthreads();
