@@ -14,7 +14,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libfs_b200.so")
 OBJ_DIR = os.path.join(os.path.dirname(HERE), "_build")
 SOURCES = ["fs_api.cu", "passes.cu", "batched.cu", "batched_tc.cu", "fused.cu", "fused_log.cu", "resident.cu", "persistent.cu", "shard.cu", "setup.cu", "col_pass_static.cu", "implicit.cu",
-           "router.cu", "router_duals.cu", "mx4.cu", "mx4_product.cu"]
+           "router.cu", "router_duals.cu", "router_duals_bf16.cu", "router_duals_f16.cu", "mx4.cu", "mx4_product.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-std=c++17",
               "-Xcompiler", "-fPIC"]
 
@@ -52,7 +52,8 @@ def build(force: bool = False, verbose: bool = False, debug: bool = False) -> st
                 cmd.insert(1, "-Xptxas=-v")
             jobs.append(cmd)
     if jobs:
-        # the translation units do not depend on each other; the router's template instances take the longest
+        # the translation units do not depend on each other; the router's template instances take the longest, so they go first
+        jobs.sort(key=lambda cmd: "router" not in cmd[-3])
         with ThreadPoolExecutor(max_workers=os.cpu_count() or 1) as pool:
             list(pool.map(lambda cmd: subprocess.run(cmd, check=True), jobs))
         rebuilt = True

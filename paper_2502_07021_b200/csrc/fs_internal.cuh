@@ -9,7 +9,7 @@
 //   implicit.cu        passes with the kernel formed on the fly from point clouds (tcgen05 + ex2); tcgen05_ptx.cuh
 //   shard.cu           row-partitioned shards for several GPUs (fs_shard_*)
 //   col_pass_static.cu column half-step without any allocation
-//   router.cu          expert selection, gates, balance loss and gradient, dispatch;  router_duals.cu  its balance
+//   router.cu          expert selection, gates, balance loss and gradient, dispatch;  router_duals*.cu{,h}  its balance
 //   mx4.cu             microscaled 4-bit rounding;  mx4_product.cu  grouped product of such matrices (tcgen05)
 //   setup.cu           one-off and O(n) helpers;  cluster_ptx.cuh  PTX wrappers of the cluster kernels
 #pragma once

@@ -258,13 +258,6 @@ template <typename F, typename T, bool VEC> cudaError_t by_experts_wide(F &f, in
     if (E <= 512) return f.template run<T, 32, 16, VEC>();
     return f.template run<T, 32, 32, VEC>();
 }
-template <typename F> cudaError_t by_type_wide(F &f, int dtype, int E, bool vec) {
-    switch (dtype) {
-    case FS_F32: return vec ? by_experts_wide<F, float, true>(f, E) : by_experts_wide<F, float, false>(f, E);
-    case FS_BF16: return vec ? by_experts_wide<F, __nv_bfloat16, true>(f, E) : by_experts_wide<F, __nv_bfloat16, false>(f, E);
-    default: return vec ? by_experts_wide<F, __half, true>(f, E) : by_experts_wide<F, __half, false>(f, E);
-    }
-}
 inline int type_size(int dtype) { return dtype == FS_F32 ? 4 : 2; }
 // rows that start on 16-byte boundaries (the widest load of any instance)
 inline bool rows_aligned(const void *p, int64_t ld, int dtype) {
