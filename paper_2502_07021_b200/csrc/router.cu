@@ -15,7 +15,7 @@
 // losses.  One block finishes by itself, up to eight form a cluster whose first block reads the others' sums.  Floating sums never meet an atomic; the integer counts do, where
 // order does not matter.
 //
-// Backward.  One sweep per token: p = 2^((l - lse) log2 e), the gate terms scattered into a per-group row in shared
+// Backward.  One sweep per token: p = 2^((l - lse) log2 e) / its sum, the gate terms scattered into a per-group row in shared
 // memory (topk stores, cleared again after use), F = sum p load by a group reduction, and
 //      dl = direct + p (S (load - F) + Z - a)
 // with S = d0 E / T', Z = 2 d1 lse / T' and the gate's constants; logits are read once and the gradient written once.
@@ -589,28 +589,33 @@ __global__ void __launch_bounds__(kThreads) router_backward_kernel(const Backwar
                 direct[e] = A.normalize ? A.gate[t * A.topk + j] * (dw - a) : dw;
             }
         }
-        Pair p[NE / 2], f2 = pair(0.f, 0.f);
+        // p up to a factor that the row shares: lse is rounded at its own size, by more than log E where the logits are very
+        // large (rows of the type's lowest value), so the row's sum is formed again
+        Pair p[NE / 2], f2 = pair(0.f, 0.f), s2 = pair(0.f, 0.f);
         const Pair log2e2 = pair(kLog2e, kLog2e), lse2 = pair(-lse, -lse);
 #pragma unroll
         for (int i = 0; i < NE / 2; ++i) {
             float lo, hi;
             split(mul2(add2(pair(x[2 * i], x[2 * i + 1]), lse2), log2e2), lo, hi);
             p[i] = pair(ex2(lo), ex2(hi));
+            s2 = add2(s2, p[i]);
             f2 = fma2(p[i], share[i], f2);
         }
-        float F, F1;
+        float F, F1, sum, sum1;
         split(f2, F, F1);
+        split(s2, sum, sum1);
         F = group_sum<G>(F + F1);
+        sum = group_sum<G>(sum + sum1);
+        const float inv = sum != 0.f ? rcp(sum) : 0.f; // 0: a row that is not active; NaN where the row holds one
         __syncwarp();
-        const float base = fmaf(Zc, lse, -F) - (A.normalize ? 0.f : a);
-        const Pair base2 = pair(base, base);
+        const float base = inv * (fmaf(Zc, lse, -F * inv) - (A.normalize ? 0.f : a));
+        const Pair inv2 = pair(inv, inv), base2 = pair(base, base);
         float d[NE], own_v[NE];
         Map::read(direct, sub, own_v);
 #pragma unroll
         for (int i = 0; i < NE / 2; ++i) {
             const Pair own = pair(own_v[2 * i], own_v[2 * i + 1]);
-            Pair g = add2(share[i], base2);
-            g = A.normalize ? fma2(p[i], g, own) : mul2(p[i], add2(g, own));
+            const Pair g = A.normalize ? fma2(p[i], fma2(share[i], inv2, base2), own) : mul2(p[i], fma2(add2(share[i], own), inv2, base2));
             split(g, d[2 * i], d[2 * i + 1]);
         }
         if (in) Map::store(to, E, sub, d);

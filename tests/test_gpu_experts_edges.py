@@ -4,8 +4,9 @@ Tolerances are those of test_gpu_experts.py, derived there; where a case adds to
 import numpy as np
 import pytest
 
+import experts_ref as ref
 from paper_2502_07021_b200 import binding as fs
-from test_gpu_experts import ROUND, TYPES, dev, host, quantized, t_
+from test_gpu_experts import ROUND, TYPES, dev, host, quantized, run_forward, t_
 
 pytestmark = pytest.mark.gpu
 
@@ -35,3 +36,60 @@ def test_product_of_a_slice_of_the_groups(first, sizes, outs, cols):
         assert np.all(got[:first] == 0) and np.all(got[off[groups]:] == 0)
         assert np.all(np.abs(got - want) <= (cols / 64 + 4) * 2.0 ** -22 * size + 1.01 * ROUND[dtype] * np.abs(want) + 2.0 ** -25 * (size > 0))
         assert torch.all(y[:, outs:] == 7.0)
+
+
+# ---- gradient -------------------------------------------------------------------------------------------------
+def gradient_64(l, idx, k, normalize, load, d_gate, d_loss):
+    """The gradient with probabilities from differences to the row's maximum, which no size of the logits hurts."""
+    t, e = l.shape
+    m = l.max(1, keepdims=True)
+    w = np.exp(l - m)
+    s = w.sum(1, keepdims=True)
+    p, lse = w / s, (m + np.log(s))[:, 0]
+    dw = np.zeros((t, e))
+    np.put_along_axis(dw, idx, d_gate, 1)
+    if normalize:
+        chosen = np.zeros((t, e))
+        np.put_along_axis(chosen, idx, 1.0, 1)
+        z = np.where(chosen > 0, l, -np.inf)
+        q = np.exp(z - z.max(1, keepdims=True))
+        q /= q.sum(1, keepdims=True)
+    else:
+        q = p
+    d = q * (dw - (q * dw).sum(1, keepdims=True))
+    d += d_loss[0] * e / t * p * (load - p @ load[:, None])
+    return d + d_loss[1] * 2 / t * lse[:, None] * p, p, lse
+
+
+@pytest.mark.parametrize("normalize", [True, False])
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("e", [10, 60, 256, 600])
+def test_gradient_of_rows_of_large_numbers(e, dtype, normalize):
+    """Rows filled with the type's lowest value share evenly (p = 1/E), and rows moved by 1e4 have the p of their differences."""
+    import torch
+    rng = np.random.default_rng(e)
+    t, k = 300, 4
+    l = rng.standard_normal((t, e)) * 1.5
+    l[1::3] += 1e4
+    l[2::9] -= 2e4
+    x = dev(l, t_(dtype))
+    x[::5] = torch.finfo(x.dtype).min
+    x[5::25, e // 2] = 1.0                          # among them rows with one expert open
+    l32 = x.float().cpu().numpy()
+    idx = ref.select(l32, None, None, k)
+    o = run_forward(x, None, None, k, normalize)
+    assert np.array_equal(o["idx"].cpu().numpy(), idx)
+    load = host(o["load"])
+    dg = rng.standard_normal((t, k)).astype(np.float32)
+    # the second loss's gradient is of the size of lse itself, so it gets a run without those rows
+    for dl in (np.array([1.0, 0.0], np.float32) * t, np.array([0.5, 1e-3], np.float32) * t):
+        out = torch.full((t, e), float("nan"), dtype=x.dtype, device="cuda")
+        fs.fs_router_backward(x, fs.fs_dtype(x), e, t, e, None, k, 1 if normalize else 0, o["idx"], o["gate"], o["lse"], o["counts"],
+                              o["load"], dev(dg), dev(dl), out, e, None)
+        want, p, lse = gradient_64(l32.astype(np.float64), idx, k, normalize, load, dg.astype(np.float64), dl.astype(np.float64))
+        bound = np.abs(dg).max() * k + p * (dl[0] * e / t * load.max() * 2 + dl[1] * 2 / t * np.abs(lse)[:, None])
+        rows = np.ones(t, bool)
+        if dl[1]:
+            rows[::5] = False
+        tol = 1e-5 * bound + ROUND[dtype] * 1.01 * np.abs(want) + 2.0 ** -24
+        assert np.all(np.abs(host(out) - want)[rows] <= tol[rows])
