@@ -382,7 +382,8 @@ int fs_debug_report(int32_t *checked_build, int64_t *canary_failures, int64_t *l
  *   logits_dev, dtype, ld   DEVICE [tokens][experts] of type `dtype` (FS_F32, FS_BF16, FS_F16), rows ld >= experts
  *                           elements apart.  1 <= experts <= FS_ROUTER_MAX_EXPERTS (FS_ERR_TOO_LARGE beyond); tokens >= 0.
  *                           -inf closes an expert to a token.  NaN and +inf act as in a softmax: the row's results are
- *                           NaN (and the balance's); the selection passes over a NaN.
+ *                           NaN (and the balance's); the selection passes over a NaN, but the gates of that row are NaN in
+ *                           all places.
  *   mask_dev                DEVICE [tokens] bytes or NULL: rows with 0 are padding, their logits are never used.
  * A row is ACTIVE when it is not masked and some entry is > -inf; T' below is the number of active rows.  All sums,
  * maxima and exponentials are taken in fp32 whatever the type; sums over tokens in a fixed order (bit-reproducible).
@@ -417,10 +418,12 @@ int fs_router_duals(const void *logits_dev, int dtype, int64_t ld, int64_t token
 /*
  * fs_router_forward -- selection, gates, and the balance loss with its counts.
  *   bias_dev   DEVICE [experts] fp32 or NULL.  Token t takes the topk largest scores l_te + bias_e (one fp32 addition; only
- *              those > -inf; ties go to the lower expert).  1 <= topk <= min(experts, FS_ROUTER_MAX_TOPK).
+ *              those > -inf; ties go to the lower expert).  1 <= topk <= min(experts, FS_ROUTER_MAX_TOPK).  An expert whose
+ *              bias is NaN is passed over, and every gate of every active row is then NaN (as duals that are no numbers are
+ *              passed on).
  *   idx_out    DEVICE [tokens][topk] int32, best first; -1 where fewer experts were open.
  *   gate_out   DEVICE [tokens][topk] fp32: softmax_e(l_t) at the chosen experts (the bias takes no part), 0 where
- *              idx is -1; with FS_ROUTE_NORMALIZE divided by their sum.
+ *              idx is -1; with FS_ROUTE_NORMALIZE divided by their sum.  All NaN in an active row with a NaN (see above).
  *   lse_out    DEVICE [tokens] or NULL: log sum_e exp l_te, 0 for rows that are not active.
  *   counts_out DEVICE [experts + 1] int32 or NULL: tokens that chose each expert; the last entry is T'.
  *   load_out   DEVICE [experts] or NULL: counts_e / (topk T').

@@ -110,7 +110,7 @@ __global__ void __launch_bounds__(forward_threads<NE>(), NE <= 8 ? 2 : 1) router
     float *logit_of = reinterpret_cast<float *>(smem + (size_t)GROUPS * A.topk * sizeof(float2) + (G >= 16 ? 8 * kThreads : 0)) + (threadIdx.x / G) * G;
     int *cnt = reinterpret_cast<int *>(smem + (size_t)GROUPS * A.topk * sizeof(float2) + (G >= 16 ? 12 * kThreads : 0));
     float *red = reinterpret_cast<float *>(cnt + A.E);
-    __shared__ float red_w[kWarps];
+    __shared__ float red_w[kWarps], lost[kWarps]; // lost: NaN where the bias holds one, else 0; one copy per warp
     const int E = A.E, sub = threadIdx.x % G, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int base = lane & ~(G - 1); // the group's first lane
     const T *logits = static_cast<const T *>(A.logits);
@@ -146,6 +146,12 @@ __global__ void __launch_bounds__(forward_threads<NE>(), NE <= 8 ? 2 : 1) router
         row += step * A.ld;
     };
     fetch(t);
+    bool nan = false; // asked with the first row under way
+#pragma unroll
+    for (int i = 0; i < NE; ++i) nan |= bias[i] != bias[i];
+    nan = __any_sync(0xffffffffu, nan); // a group's lanes have all columns
+    if (lane == 0) lost[warp] = nan ? NAN : 0.f;
+    __syncwarp();
     int32_t *idx_t = A.idx + t * A.topk;
     float *gate_t = A.gate + t * A.topk;
     // every lane of a warp makes the same number of rounds (the shuffles name the whole warp)
@@ -246,8 +252,8 @@ __global__ void __launch_bounds__(forward_threads<NE>(), NE <= 8 ? 2 : 1) router
                         w = ex2((l - top) * kLog2e);
                         const float all = group_sum<G>(w);
                         scale = all > 0.f ? rcp(all) : 0.f;
-                        if (on && !(sum == sum)) scale = sum; // a NaN in the row reaches its gates
                     }
+                    if (on) scale += lost[warp] + (sum - sum); // a NaN in the row or in the bias reaches all its gates
                     if (in) {
                         if (take) {
                             const int e = (int)~(uint32_t)key;
@@ -255,7 +261,7 @@ __global__ void __launch_bounds__(forward_threads<NE>(), NE <= 8 ? 2 : 1) router
                             gate_t[rank] = w * scale;
                             if (A.stats) atomicAdd(&cnt[e], 1);
                         }
-                        if (sub >= n && sub < A.topk) idx_t[sub] = -1, gate_t[sub] = 0.f; // fewer than topk open
+                        if (sub >= n && sub < A.topk) idx_t[sub] = -1, gate_t[sub] = 0.f * scale; // fewer than topk open
                     }
                     __syncwarp();
                 }
@@ -323,14 +329,14 @@ __global__ void __launch_bounds__(forward_threads<NE>(), NE <= 8 ? 2 : 1) router
             float w = 0.f;
             for (int j = 0; j < A.topk; ++j) w += ex2((sel[j].y - top) * kLog2e);
             scale = w > 0.f ? rcp(w) : 0.f;
-            if (on && !(sum == sum)) scale = sum; // a NaN in the row reaches its gates
         }
+        if (on) scale += lost[warp] + (sum - sum); // as above
         if (in) {
             for (int j = sub; j < A.topk; j += G) {
                 const float2 c = sel[j];
                 const int e = __float_as_int(c.x);
                 idx_t[j] = e;
-                gate_t[j] = e >= 0 ? ex2((c.y - top) * kLog2e) * scale : 0.f;
+                gate_t[j] = (e >= 0 ? ex2((c.y - top) * kLog2e) : 0.f) * scale;
                 if (A.stats && e >= 0) atomicAdd(&cnt[e], 1);
             }
         }

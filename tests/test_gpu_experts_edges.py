@@ -93,3 +93,40 @@ def test_gradient_of_rows_of_large_numbers(e, dtype, normalize):
             rows[::5] = False
         tol = 1e-5 * bound + ROUND[dtype] * 1.01 * np.abs(want) + 2.0 ** -24
         assert np.all(np.abs(host(out) - want)[rows] <= tol[rows])
+
+
+# ---- choice ---------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("normalize", [True, False])
+@pytest.mark.parametrize("e,k", [(6, 3), (60, 4), (100, 8), (100, 12), (256, 8), (700, 32)])
+def test_a_nan_reaches_every_gate_of_its_rows(e, k, normalize):
+    """A NaN logit makes its row's gates NaN, a NaN in the bias those of every active row, places without an expert included;
+    the choice passes over both."""
+    rng = np.random.default_rng(e + k)
+    l = rng.standard_normal((40, e)).astype(np.float32)
+    l[1] = np.nan                                   # no score at all
+    l[2, :] = -np.inf
+    l[2, :2] = [np.nan, 1.0]                        # one open expert
+    l[3, e - 1] = np.nan
+    l[4] = -np.inf                                  # not active
+    l[5, k - 1:] = -np.inf                          # fewer open than wanted
+    mask = np.ones(40, np.uint8)
+    mask[[6, 39]] = 0
+    l[6] = np.nan
+    nan_rows = [1, 2, 3]
+    for bad in (False, True):
+        bias = (rng.standard_normal(e) * 0.5).astype(np.float32)
+        if bad:
+            bias[e // 2] = np.nan
+        o = run_forward(dev(l), dev(mask), dev(bias), k, normalize)
+        idx, gate = o["idx"].cpu().numpy(), host(o["gate"])
+        assert np.array_equal(idx, ref.select(l, mask, bias, k))
+        active = np.ones(40, bool)
+        active[[4, 6, 39]] = False
+        assert np.all(gate[~active] == 0)
+        assert np.all(np.isnan(gate[nan_rows]))
+        clean = np.setdiff1d(np.flatnonzero(active), nan_rows)
+        assert np.all(np.isnan(gate[clean])) if bad else np.all(np.isfinite(gate[clean]))
+        if not bad:
+            assert np.all(gate[5][idx[5] < 0] == 0)
+        lse = host(o["lse"])                        # the bias takes no part in it
+        assert np.all(np.isfinite(lse[clean])) and np.all(np.isnan(lse[nan_rows]))
