@@ -15,7 +15,7 @@
 // losses.  One block finishes by itself, up to eight form a cluster whose first block reads the others' sums.  Floating sums never meet an atomic; the integer counts do, where
 // order does not matter.
 //
-// Backward.  One sweep per token: p = 2^((l - lse) log2 e) / its sum, the gate terms scattered into a per-group row in shared
+// Backward.  One sweep per token: p = 2^((l - lse) log2 e), over its sum where lse is large, the gate terms scattered into a per-group row in shared
 // memory (topk stores, cleared again after use), F = sum p load by a group reduction, and
 //      dl = direct + p (S (load - F) + Z - a)
 // with S = d0 E / T', Z = 2 d1 lse / T' and the gate's constants; logits are read once and the gradient written once.
@@ -595,24 +595,30 @@ __global__ void __launch_bounds__(kThreads) router_backward_kernel(const Backwar
                 direct[e] = A.normalize ? A.gate[t * A.topk + j] * (dw - a) : dw;
             }
         }
-        // p up to a factor that the row shares: lse is rounded at its own size, by more than log E where the logits are very
-        // large (rows of the type's lowest value), so the row's sum is formed again
-        Pair p[NE / 2], f2 = pair(0.f, 0.f), s2 = pair(0.f, 0.f);
+        Pair p[NE / 2], f2 = pair(0.f, 0.f);
         const Pair log2e2 = pair(kLog2e, kLog2e), lse2 = pair(-lse, -lse);
 #pragma unroll
         for (int i = 0; i < NE / 2; ++i) {
             float lo, hi;
             split(mul2(add2(pair(x[2 * i], x[2 * i + 1]), lse2), log2e2), lo, hi);
             p[i] = pair(ex2(lo), ex2(hi));
-            s2 = add2(s2, p[i]);
             f2 = fma2(p[i], share[i], f2);
         }
-        float F, F1, sum, sum1;
+        float F, F1;
         split(f2, F, F1);
-        split(s2, sum, sum1);
         F = group_sum<G>(F + F1);
-        sum = group_sum<G>(sum + sum1);
-        const float inv = sum != 0.f ? rcp(sum) : 0.f; // 0: a row that is not active; NaN where the row holds one
+        // lse is rounded at its own size: below 16 that costs every p less than 5e-7, in a row of the type's lowest value lse
+        // equals the entries and every p is 1.  So rows beyond that have their powers summed again.
+        float inv = 1.f;
+        if (__any_sync(0xffffffffu, fabsf(lse) > 16.f)) {
+            Pair s2 = p[0];
+#pragma unroll
+            for (int i = 1; i < NE / 2; ++i) s2 = add2(s2, p[i]);
+            float sum, sum1;
+            split(s2, sum, sum1);
+            sum = group_sum<G>(sum + sum1);
+            if (fabsf(lse) > 16.f) inv = rcp(sum); // by the row's own lse: what shares the warp changes nothing
+        }
         __syncwarp();
         const float base = inv * (fmaf(Zc, lse, -F * inv) - (A.normalize ? 0.f : a));
         const Pair inv2 = pair(inv, inv), base2 = pair(base, base);
