@@ -6,8 +6,8 @@
 // -- r after the update is -f_t, the row half-step -- and each lane adds P into its NE running column sums.  Any r
 // gives the same P; the r of the iteration before keeps sum p near 1 without a maximum over the row, and a sum outside
 // 2^-20 .. 2^20 (g moved far) sends the row once more through the maximum.  c_e = sum_t P_te is all that the column
-// half-step needs: g_e += eps (log(T' b_e) - log c_e).  A c_e too small for the sums' resolution is redone in the log
-// domain, maximum first, before it is used, so the update never sees an underflowed sum.
+// half-step needs: g_e += eps (log(T' b_e) - log c_e).  A c_e that flushed powers or the sums' resolution could touch by more than
+// 2^-20 of itself is redone in the log domain, maximum first, before it is used.
 //
 // All iterations run in one launch; as many rows as fit stay in shared memory in their own type, the rest is read again
 // from L2.  How the blocks' column sums meet goes by the number of rows.  One block: __syncthreads.  One cluster of up to 16
@@ -49,7 +49,9 @@ cudaError_t run_duals_f16(const DualsArgs &A, bool vec, cudaStream_t st);
 namespace {
 
 constexpr uint32_t kPollLimit = 1u << 21;
-constexpr float kStarved = 1e-30f;    // one block: column sums are fp32
+// A column sum below n kHidden is redone in the log domain.  Powers below 2^-126 are flushed, and in a row whose powers sum to as
+// little as kSumLow that hides up to 2^-106 of a column; n rows hide less than 2^-20 of a sum that is n 2^-86 or more.
+constexpr float kHidden = 1.2924697e-26f; // 2^-86
 constexpr float kSumLow = 9.5367e-7f, kSumHigh = 1048576.f; // 2^-20, 2^20
 constexpr int kMaxThreads = 512;
 constexpr int kSmemBudget = 220 * 1024;
@@ -273,8 +275,13 @@ __global__ void __launch_bounds__(kMaxThreads, 1) router_duals_kernel(const Dual
         // `parts` neighbouring lanes share a column of the warps' sums
         unsigned long long *total = A.total + (size_t)(it % 3) * (kLevels * E + 2);
         if (first && MODE == kAlone) n = n_s;
-        const float low = MODE != kGrid ? kStarved : (float)blocks * ldexpf(1.f, kLevelBits - A.fix - kLevelBits * (kLevels - 1));
         int starved = 0;
+        float low = 0.f;
+        auto set_low = [&]() { // n is known
+            low = (float)max(n, 1) * kHidden;
+            if (MODE == kGrid) low = fmaxf(low, (float)blocks * ldexpf(1.f, kLevelBits - A.fix - kLevelBits * (kLevels - 1)));
+        };
+        if (MODE == kAlone) set_low();
         auto half_step = [&](int e, float c) {
             if (first) {
                 want[e] = (float)n * (A.target ? A.target[e] : 1.f / (float)E);
@@ -317,6 +324,7 @@ __global__ void __launch_bounds__(kMaxThreads, 1) router_duals_kernel(const Dual
             cluster_sync(); // a block that is ahead writes the other buffer; it meets this one before it writes this buffer again
             if (first)
                 for (int b = 0; b < blocks; ++b) n += __float_as_int(remote(reinterpret_cast<const float *>(&n_s), b));
+            set_low();
             for (int e = threadIdx.x; e < E; e += nthreads) {
                 float v[kClusterBlocks], c = 0.f;
 #pragma unroll
@@ -331,6 +339,7 @@ __global__ void __launch_bounds__(kMaxThreads, 1) router_duals_kernel(const Dual
             if (!ok) break;
             const bool nan = __ldcg(total + kLevels * E) != 0;
             if (first) n = (int)__ldcg(total + kLevels * E + 1);
+            set_low();
             for (int e = threadIdx.x; e < E; e += nthreads) {
                 unsigned long long v[kLevels];
 #pragma unroll

@@ -6,7 +6,7 @@ import pytest
 
 import experts_ref as ref
 from paper_2502_07021_b200 import binding as fs
-from test_gpu_experts import ROUND, TYPES, dev, host, quantized, run_forward, t_
+from test_gpu_experts import ROUND, TYPES, dev, host, quantized, run_forward, scratch, t_
 
 pytestmark = pytest.mark.gpu
 
@@ -130,3 +130,27 @@ def test_a_nan_reaches_every_gate_of_its_rows(e, k, normalize):
             assert np.all(gate[5][idx[5] < 0] == 0)
         lse = host(o["lse"])                        # the bias takes no part in it
         assert np.all(np.isfinite(lse[clean])) and np.all(np.isnan(lse[nan_rows]))
+
+
+# ---- balance --------------------------------------------------------------------------------------------------
+def run_duals(x, eps, iters, mask=None, start=None):
+    import torch
+    t, e = x.shape
+    w, n = scratch(t, e, 1)
+    f, g, err = torch.full((t,), 9.0, device="cuda"), torch.full((e,), 9.0, device="cuda"), torch.full((iters,), 9.0, device="cuda")
+    fs.fs_router_duals(x, fs.fs_dtype(x), x.stride(0), t, e, mask, None, eps, iters, start, f, g, err, w, n, None)
+    return f, g, err
+
+
+def test_column_sum_of_many_powers_below_the_smallest():
+    """A column whose sum comes from one row while 60000 others add powers too small to be kept: what they add, 4e-4 of it,
+    counts."""
+    t, eps = 60001, 1.0
+    l = np.zeros((t, 3), np.float32)
+    l[:, 1] = -1.0
+    l[:, 2] = -87.4                                   # 2^-126.1
+    l[17, 2] = -68.5                                  # 2^-98.8
+    f, g, _ = run_duals(dev(l), eps, 1)
+    rf, rg, _ = ref.duals(l.astype(np.float64), None, None, eps, 1)
+    assert np.all(np.abs(host(g) - rg) <= 4e-6 * 2 * (1 + np.abs(rg) / 16))
+    assert np.all(np.abs(host(f) - rf) <= 4e-6 * 2 * (1 + np.abs(rf) / 16))
