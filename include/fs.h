@@ -402,6 +402,7 @@ int64_t fs_router_workspace(int64_t tokens, int32_t experts, int32_t topk);
  * fs_router_duals -- `iters` >= 1 Sinkhorn iterations in the log domain between the active rows (one unit each) and the
  * experts (T' b_e each), from g = g_start (0 if NULL):
  *      f_t <- -eps LSE_e((l_te + g_e)/eps),      g_e <- eps log(T' b_e) - eps LSE_t((l_te + f_t)/eps).
+ *   eps          > 0, with eps and log2(e)/eps inside fp32's range (FS_ERR_BAD_EPS otherwise).
  *   target_dev   DEVICE [experts] shares b_e > 0 (not checked; their sum should be 1), or NULL for 1/experts each.
  *   g_start_dev  DEVICE [experts] finite duals to continue from, or NULL.
  *   f_out_dev    DEVICE [tokens] or NULL: f of the last iteration, 0 for rows that are not active.

@@ -11,7 +11,8 @@ extern "C" int fs_router_duals(const void *logits_dev, int dtype, int64_t ld, in
     if ((tokens > 0 && !logits_dev) || !g_out_dev || !work_dev) return FS_ERR_NULL;
     if ((dtype != FS_F32 && dtype != FS_BF16 && dtype != FS_F16) || tokens < 0 || experts < 1 || (tokens > 1 && ld < experts) || iters < 1)
         return FS_ERR_BAD_N;
-    if (!(eps > 0) || !isfinite(eps) || !isfinite(1.4426950408889634 / (double)(float)eps)) return FS_ERR_BAD_EPS;
+    // eps and log2(e) / eps are used as fp32
+    if (!(eps > 0) || !isfinite((float)eps) || !((float)eps > 0) || !isfinite((float)(1.4426950408889634 / eps))) return FS_ERR_BAD_EPS;
     if (experts > FS_ROUTER_MAX_EXPERTS || tokens > INT32_MAX || work_bytes < workspace_bytes(tokens, experts, 1))
         return FS_ERR_TOO_LARGE;
     if ((reinterpret_cast<uintptr_t>(work_dev) & 15) || reinterpret_cast<uintptr_t>(logits_dev) % type_size(dtype))
