@@ -132,6 +132,29 @@ def test_a_nan_reaches_every_gate_of_its_rows(e, k, normalize):
         assert np.all(np.isfinite(lse[clean])) and np.all(np.isnan(lse[nan_rows]))
 
 
+@pytest.mark.parametrize("e,k", [(6, 2), (40, 5), (65, 8), (100, 8), (128, 7), (128, 16), (256, 8), (256, 16), (256, 20), (500, 8), (1000, 12)])
+def test_ties_zeros_and_nan_at_every_width(e, k):
+    """Equal scores go to the lower expert in every form of the choice: few ties, more ties than candidates are kept, all equal;
+    -0 equals 0; a NaN is passed over."""
+    rng = np.random.default_rng(e * 31 + k)
+    few = rng.standard_normal((60, e))
+    some = np.round(rng.standard_normal((60, e)) * 2)           # small whole numbers
+    many = rng.integers(0, 2, (60, e)).astype(float)
+    same = np.zeros((20, e))
+    signs = np.where(rng.random((40, e)) < 0.5, -0.0, 0.0)
+    signs[rng.random((40, e)) < 0.02] = 1.0
+    edge = np.round(rng.standard_normal((60, e)))
+    edge[rng.random((60, e)) < 0.3] = -np.inf
+    edge[rng.random((60, e)) < 0.3] = np.nan
+    edge[7] = np.nan
+    l = np.concatenate([few, some, many, same, signs, edge])
+    for dtype in TYPES:
+        for bias in (None, np.round(rng.standard_normal(e)).astype(np.float32)):
+            x = dev(l, t_(dtype))
+            o = run_forward(x, None, None if bias is None else dev(bias), k, True)
+            assert np.array_equal(o["idx"].cpu().numpy(), ref.select(x.float().cpu().numpy(), None, bias, k))
+
+
 # ---- balance --------------------------------------------------------------------------------------------------
 def run_duals(x, eps, iters, mask=None, start=None):
     import torch
@@ -154,3 +177,62 @@ def test_column_sum_of_many_powers_below_the_smallest():
     rf, rg, _ = ref.duals(l.astype(np.float64), None, None, eps, 1)
     assert np.all(np.abs(host(g) - rg) <= 4e-6 * 2 * (1 + np.abs(rg) / 16))
     assert np.all(np.abs(host(f) - rf) <= 4e-6 * 2 * (1 + np.abs(rf) / 16))
+
+
+# more sweeps over the rows than one cluster of sixteen blocks makes (eight each): the balance meets on the whole grid
+GRID = [(70001, 12), (33000, 30), (17001, 40), (8500, 128), (5001, 256), (2500, 500), (2300, 1024)]
+
+
+@pytest.mark.parametrize("t,e", GRID)
+def test_balance_on_the_grid_with_starved_and_closed_experts(t, e):
+    rng = np.random.default_rng(t)
+    l = rng.standard_normal((t, e)).astype(np.float32)
+    l[:, 3] -= 60.0
+    l[:, 7] = -np.inf
+    l[5] = -np.inf
+    mask = (rng.random(t) >= 0.05).astype(np.uint8)
+    l[mask == 0] = np.nan
+    g0 = (rng.standard_normal(e) * 0.1).astype(np.float32)
+    f, g, err = run_duals(dev(l), 0.1, 5, dev(mask), dev(g0))
+    rf, rg, rerr = ref.duals(np.nan_to_num(l.astype(np.float64), nan=0.0, neginf=-np.inf), mask, None, 0.1, 5, g0.astype(np.float64))
+    assert host(g)[7] == g0[7]
+    # the starved column's dual is of size 60: its exponents are rounded at that size
+    assert np.all(np.abs(host(g) - rg) <= 4e-6 * 6 * (1 + np.abs(rg) / 16) * 4)
+    assert np.all(np.abs(host(f) - rf) <= 4e-6 * 6 * 4 * (1 + np.abs(rf) / 16))
+    assert np.all(np.abs(host(err) - rerr) <= 1e-5 + 2 * 4e-6 * 6 * 4 / 0.1)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("t,e", GRID)
+def test_balance_on_the_grid_of_column_sums_of_every_size(t, e, dtype):
+    """Columns from 1 down to 1e-24 of a share at the start, so that every level of the common sums is used."""
+    rng = np.random.default_rng(t + 1)
+    eps, iters = 0.4, 4
+    l = rng.standard_normal((t, e)) * 0.3 - eps * np.log(10.0) * np.linspace(0, 24, e)
+    x = dev(l, t_(dtype))
+    f, g, err = run_duals(x, eps, iters)
+    again = run_duals(x, eps, iters)
+    assert all(np.array_equal(host(a), host(b)) for a, b in zip((f, g, err), again))
+    rf, rg, rerr = ref.duals(host(x), None, None, eps, iters)
+    tol = 4e-6 * (1 + iters)
+    assert np.all(np.abs(host(f) - rf) <= tol * (1 + np.abs(rf) / 16))
+    assert np.all(np.abs(host(g) - rg) <= tol * (1 + np.abs(rg) / 16))
+    assert np.all(np.abs(host(err) - rerr) <= 1e-5 + 2 * tol / eps)
+
+
+@pytest.mark.parametrize("t,e", GRID)
+def test_balance_on_the_grid_with_rows_of_the_lowest_value_and_nan(t, e):
+    rng = np.random.default_rng(t + 2)
+    l = rng.standard_normal((t, e)).astype(np.float32)
+    low = np.zeros(t, bool)
+    low[::7] = True
+    l[low] = np.finfo(np.float32).min
+    l[3::11, 5] = np.finfo(np.float32).min
+    f, g, _ = run_duals(dev(l), 0.05, 4)
+    rf, rg, _ = ref.duals(l.astype(np.float64), None, None, 0.05, 4)
+    assert np.all(np.abs(host(g) - rg) <= 4e-6 * 5 * (1 + np.abs(rg) / 16))
+    assert np.all(np.abs(host(f) - rf)[~low] <= 4e-6 * 5 * (1 + np.abs(rf[~low]) / 16))
+    assert np.allclose(host(f)[low], rf[low], rtol=1e-6)
+    l[t - 1, e - 1] = np.nan                          # one active row with a NaN: nothing of the balance is a number
+    f, g, err = run_duals(dev(l), 0.05, 2)
+    assert np.all(np.isnan(host(g))) and np.all(np.isnan(host(err))) and np.all(np.isnan(host(f)))
