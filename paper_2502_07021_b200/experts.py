@@ -24,6 +24,12 @@ def _scratch(tokens, experts, topk, device):
     return torch.empty(size, dtype=torch.uint8, device=device), size
 
 
+def _rows(x):
+    """x itself where its rows lie one after another with their entries side by side, else a copy that does."""
+    ok = (x.shape[1] < 2 or x.stride(1) == 1) and (x.shape[0] < 2 or x.stride(0) >= x.shape[1])
+    return x if ok else x.contiguous()
+
+
 def _scores(logits):
     if logits.dim() != 2 or not logits.is_cuda:
         raise ValueError("logits: a CUDA tensor [tokens, experts]")
@@ -103,7 +109,7 @@ def route(logits, topk, bias=None, mask=None, normalize=True):
 
 def quantize(x):
     """(codes, scale bytes) of a matrix or a stack [groups, rows, cols] of them, on the 4-bit microscaled grid."""
-    flat = x.reshape(-1, x.shape[-1])
+    flat = _rows(x.reshape(-1, x.shape[-1]))
     q, s = fs.mx4_empty(flat.shape[0], flat.shape[1], x.device)
     fs.fs_mx4_quantize(flat, fs.fs_dtype(flat), flat.stride(0), flat.shape[0], flat.shape[1], None, 1, flat.shape[0], q, q.stride(0),
                        s, s.stride(0), torch.cuda.current_stream(x.device))
@@ -131,6 +137,9 @@ class RoutedExperts:
         self.up, self.down = quantize(up), quantize(down)   # laid out once
 
     def __call__(self, x, mask=None):
+        if x.dim() != 2 or x.shape[1] != self.width:
+            raise ValueError("x: [tokens, width]")
+        x = _rows(x)
         tokens, experts = x.shape[0], self.score.shape[0]
         stream = torch.cuda.current_stream(x.device)
         logits = x @ self.score.T

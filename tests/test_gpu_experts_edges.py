@@ -236,3 +236,42 @@ def test_balance_on_the_grid_with_rows_of_the_lowest_value_and_nan(t, e):
     l[t - 1, e - 1] = np.nan                          # one active row with a NaN: nothing of the balance is a number
     f, g, err = run_duals(dev(l), 0.05, 2)
     assert np.all(np.isnan(host(g))) and np.all(np.isnan(host(err))) and np.all(np.isnan(host(f)))
+
+
+# ---- the layer and the wrappers -------------------------------------------------------------------------------
+def make_layer(experts, width=64, hidden=96, k=2, dtype="bfloat16", seed=3, **kw):
+    import torch
+    from paper_2502_07021_b200.experts import RoutedExperts
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(seed)
+    r = lambda *s: torch.randn(*s, device="cuda", generator=gen)
+    return RoutedExperts((r(experts, width) / width ** 0.5).to(t_(dtype)), (r(experts, hidden, width) / width ** 0.5).to(t_(dtype)),
+                         (r(experts, width, hidden) / hidden ** 0.5).to(t_(dtype)), k, **kw)
+
+
+def tokens_of(n, width=64, dtype="bfloat16", seed=4):
+    import torch
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(seed)
+    return torch.randn(n, width, device="cuda", generator=gen).to(t_(dtype))
+
+
+def test_strided_activations_and_weights():
+    import torch
+    from paper_2502_07021_b200 import experts
+    wide = tokens_of(70, 128)
+    views = [wide[:, ::2], wide[:, 1::2], wide[:64].t()[:64], wide[:1, :64].expand(70, 64), wide[3:4, 64:], wide[:, 5:69]]
+    for v in views:
+        q, s = experts.quantize(v)
+        q2, s2 = experts.quantize(v.clone(memory_format=torch.contiguous_format))
+        assert torch.equal(q, q2) and torch.equal(s, s2)
+    stack = torch.randn(3, 40, 128, device="cuda")
+    for v in (stack[:, :, ::2], stack.transpose(1, 2), stack[:, ::3], stack[::2]):
+        q, s = experts.quantize(v)
+        q2, s2 = experts.quantize(v.contiguous())
+        assert q.shape[:-1] == v.shape[:-1] and torch.equal(q, q2) and torch.equal(s, s2)
+    layer = make_layer(12, k=3)
+    for v in views[:4]:
+        y, idx = layer(v)
+        y2, idx2 = layer(v.contiguous())
+        assert torch.equal(idx, idx2) and torch.equal(y, y2)
