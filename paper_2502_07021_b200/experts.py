@@ -38,12 +38,38 @@ def _scores(logits):
     return logits.shape[0], logits.shape[1], fs.fs_dtype(logits)
 
 
-def _mask(mask, tokens):
+def _mask(mask, logits):
     if mask is None:
         return None
-    if mask.shape != (tokens,) or mask.dtype not in (torch.uint8, torch.bool):
+    if mask.shape != logits.shape[:1] or mask.dtype not in (torch.uint8, torch.bool):
         raise ValueError("mask: one byte or truth value per token")
+    _together(logits.device, mask=mask)
     return mask.view(torch.uint8).contiguous()
+
+
+def _per_expert(v, name, logits):
+    if v is None:
+        return None
+    if v.shape != logits.shape[1:] or v.dtype != torch.float32:
+        raise ValueError(f"{name}: float32 [experts]")
+    _together(logits.device, **{name: v})
+    return v.contiguous()
+
+
+def _together(device, **tensors):
+    for name, t in tensors.items():
+        if t is not None and t.device != device:
+            raise ValueError(f"{name}: on {t.device}, expected {device}")
+
+
+def _packed(t, name, lead, need):
+    """Distance in bytes between the rows of codes or scale bytes [..., >= need], rows of a stack all equally far apart."""
+    if t.dtype != torch.uint8 or t.shape[:-1] != lead or t.shape[-1] < need or (t.shape[-1] > 1 and t.stride(-1) != 1):
+        raise ValueError(f"{name}: uint8 {[*lead]} rows of {need} bytes or more")
+    if len(lead) == 2 and min(lead) > 1 and t.stride(0) != lead[1] * t.stride(1):
+        raise ValueError(f"{name}: a stack whose matrices follow one another")
+    apart = [d for d in range(len(lead)) if lead[d] > 1]
+    return t.stride(apart[-1]) if apart else -(-need // 4) * 4      # one row: no distance
 
 
 def balance(logits, eps, iters, mask=None, share=None, start=None):
@@ -53,8 +79,9 @@ def balance(logits, eps, iters, mask=None, share=None, start=None):
     tokens, experts, dtype = _scores(logits)
     work, size = _scratch(tokens, experts, 1, logits.device)
     f, g, err = (torch.empty(n, device=logits.device) for n in (tokens, experts, iters))
-    fs.fs_router_duals(logits, dtype, logits.stride(0), tokens, experts, _mask(mask, tokens), share, eps, iters, start, f, g, err,
-                       work, size, torch.cuda.current_stream(logits.device))
+    fs.fs_router_duals(logits, dtype, logits.stride(0), tokens, experts, _mask(mask, logits), _per_expert(share, "share", logits),
+                       eps, iters, _per_expert(start, "start", logits), f, g, err, work, size,
+                       torch.cuda.current_stream(logits.device))
     return f, g, err
 
 
@@ -64,7 +91,7 @@ def choose(logits, topk, bias=None, mask=None, normalize=True):
     work, size = _scratch(tokens, experts, topk, logits.device)
     idx = torch.empty(tokens, topk, dtype=torch.int32, device=logits.device)
     gate = torch.empty(tokens, topk, device=logits.device)
-    fs.fs_router_forward(logits, dtype, logits.stride(0), tokens, experts, _mask(mask, tokens), bias, topk,
+    fs.fs_router_forward(logits, dtype, logits.stride(0), tokens, experts, _mask(mask, logits), _per_expert(bias, "bias", logits), topk,
                          fs.FS_ROUTE_NORMALIZE if normalize else 0, idx, gate, None, None, None, None, None, work, size,
                          torch.cuda.current_stream(logits.device))
     return idx, gate
@@ -75,7 +102,7 @@ class _Route(torch.autograd.Function):
     def forward(ctx, logits, topk, bias, mask, normalize):
         tokens, experts, dtype = _scores(logits)
         dev = logits.device
-        mask = _mask(mask, tokens)
+        mask, bias = _mask(mask, logits), _per_expert(bias, "bias", logits)
         work, size = _scratch(tokens, experts, topk, dev)
         idx = torch.empty(tokens, topk, dtype=torch.int32, device=dev)
         counts = torch.empty(experts + 1, dtype=torch.int32, device=dev)
@@ -117,11 +144,20 @@ def quantize(x):
 
 
 def product(xq, xs, weights, offsets, cols, dtype):
-    """Rows ordered by group times their group's 4-bit weights (codes, scales) [groups, outs, ...]."""
+    """Rows ordered by group times their group's 4-bit weights (codes, scales) [groups, outs, ...]; offsets int32 [groups + 1], None for one
+    group of all rows."""
     wq, ws = weights
-    y = torch.empty(xq.shape[0], wq.shape[1], dtype=dtype, device=xq.device)
-    fs.fs_mx4_product(xq, xq.stride(0), xs, xs.stride(0), xq.shape[0], wq, wq.stride(1), ws, ws.stride(1), wq.shape[0], offsets,
-                      wq.shape[1], cols, y, fs.fs_dtype(y), y.stride(0), torch.cuda.current_stream(xq.device))
+    rows, groups, outs, nb = xq.shape[0], wq.shape[0], wq.shape[1], -(-cols // 32)
+    _together(xq.device, xs=xs, wq=wq, ws=ws, offsets=offsets)
+    if offsets is not None:
+        if offsets.dtype != torch.int32 or offsets.shape != (groups + 1,):
+            raise ValueError("offsets: int32 [groups + 1]")
+        offsets = offsets.contiguous()
+    pitches = [_packed(t, name, lead, need) for t, name, lead, need in (
+        (xq, "xq", (rows,), 16 * nb), (xs, "xs", (rows,), nb), (wq, "wq", (groups, outs), 16 * nb), (ws, "ws", (groups, outs), nb))]
+    y = torch.empty(rows, outs, dtype=dtype, device=xq.device)
+    fs.fs_mx4_product(xq, pitches[0], xs, pitches[1], rows, wq, pitches[2], ws, pitches[3], groups, offsets, outs, cols, y,
+                      fs.fs_dtype(y), y.stride(0), torch.cuda.current_stream(xq.device))
     return y
 
 
@@ -139,6 +175,7 @@ class RoutedExperts:
     def __call__(self, x, mask=None):
         if x.dim() != 2 or x.shape[1] != self.width:
             raise ValueError("x: [tokens, width]")
+        _together(x.device, score=self.score)
         x = _rows(x)
         tokens, experts = x.shape[0], self.score.shape[0]
         stream = torch.cuda.current_stream(x.device)

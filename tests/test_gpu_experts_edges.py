@@ -275,3 +275,65 @@ def test_strided_activations_and_weights():
         y, idx = layer(v)
         y2, idx2 = layer(v.contiguous())
         assert torch.equal(idx, idx2) and torch.equal(y, y2)
+
+
+def test_wrong_types_lengths_and_devices_are_refused():
+    import torch
+    from paper_2502_07021_b200 import experts
+    l = torch.randn(20, 8, device="cuda")
+    good = torch.full((8,), 0.125, device="cuda")
+    wrong = [good.bfloat16(), good.double(), good.half(), good[:7], good.repeat(2), good[None], good.cpu()]
+    for v in wrong:
+        for call in (lambda: experts.balance(l, 0.1, 2, share=v), lambda: experts.balance(l, 0.1, 2, start=v),
+                     lambda: experts.choose(l, 2, v), lambda: experts.route(l, 2, v)):
+            with pytest.raises(ValueError):
+                call()
+    mask = torch.ones(20, dtype=torch.bool, device="cuda")
+    for m in (mask.cpu(), mask[:19], mask.int(), mask[:, None]):
+        for call in (lambda: experts.balance(l, 0.1, 2, mask=m), lambda: experts.choose(l, 2, mask=m), lambda: experts.route(l, 2, mask=m)):
+            with pytest.raises(ValueError):
+                call()
+    with pytest.raises(ValueError):
+        experts.choose(l.cpu(), 2)
+    xq, xs = experts.quantize(torch.randn(10, 96, device="cuda"))
+    w = experts.quantize(torch.randn(3, 40, 96, device="cuda"))
+    off = torch.tensor([0, 4, 4, 10], dtype=torch.int32, device="cuda")
+    args = dict(xq=xq, xs=xs, weights=w, offsets=off, cols=96, dtype=torch.float32)
+    for bad in (dict(offsets=off.long()), dict(offsets=off[:3]), dict(offsets=off.cpu()), dict(offsets=off.float()), dict(xs=xs.cpu()),
+                dict(xs=xs[:9]), dict(xq=xq.int()), dict(xq=xq[:, :32]), dict(xq=xq.repeat(1, 2)[:, ::2]), dict(weights=(w[0], w[1][:2])),
+                dict(weights=(w[0].transpose(0, 1), w[1])), dict(weights=(w[0][0], w[1][0])),
+                dict(weights=(torch.cat([w[0], w[0]])[::2], w[1]))):
+        with pytest.raises(ValueError):
+            experts.product(**{**args, **bad})
+    layer = make_layer(12, k=3)
+    for bad in (tokens_of(5).cpu(), tokens_of(5, 32), tokens_of(5)[None]):
+        with pytest.raises(ValueError):
+            layer(bad)
+
+
+def test_strided_vectors_and_packed_matrices():
+    """What the wrappers accept besides contiguous tensors gives the same results."""
+    import torch
+    from paper_2502_07021_b200 import experts
+    l = torch.randn(50, 8, device="cuda")
+    wide = torch.randn(16, device="cuda")
+    mask = torch.arange(100, device="cuda") % 3 != 0
+    off = torch.tensor([0, 9, 4, 9, 4, 9, 10], dtype=torch.int32, device="cuda")
+    for a, b in ((wide[::2], wide[::2].contiguous()), (wide[3:11], wide[3:11].clone())):
+        for p, q in zip(experts.choose(l, 3, a, mask[::2]), experts.choose(l, 3, b, mask[::2].contiguous())):
+            assert torch.equal(p, q)
+        for p, q in zip(experts.balance(l, 0.3, 3, mask[::2], a.abs() + 0.1, a), experts.balance(l, 0.3, 3, mask[::2], b.abs() + 0.1, b)):
+            assert torch.equal(p, q)
+    x = torch.randn(10, 96, device="cuda")
+    for outs in (40, 1):
+        w = torch.randn(3, outs, 96, device="cuda")
+        xq, xs = experts.quantize(x)
+        wq, ws = experts.quantize(w)
+        plain = experts.product(xq, xs, (wq, ws), off[::2].contiguous(), 96, torch.float32)
+        pad = lambda t, n: torch.cat([t, torch.full((*t.shape[:-1], n), 255, dtype=torch.uint8, device="cuda")], -1)[..., :t.shape[-1]]
+        assert torch.equal(plain, experts.product(pad(xq, 16), pad(xs, 4), (pad(wq, 32), pad(ws, 8)), off[::2], 96, torch.float32))
+        for g in range(3):                             # one group, and one row at a time
+            one = experts.product(xq, xs, (wq[g:g + 1], ws[g:g + 1]), None, 96, torch.float32)
+            rows = slice(int(off[2 * g]), int(off[2 * g + 2]))
+            assert torch.equal(one[rows], plain[rows])
+            assert torch.equal(experts.product(xq[rows][:1], xs[rows][:1], (wq[g:g + 1], ws[g:g + 1]), None, 96, torch.float32), plain[rows][:1])
