@@ -192,8 +192,8 @@ class RoutedExperts:
                            xs.stride(0), stream)
         h = torch.nn.functional.silu(product(xq, xs, self.up, offsets, self.width, x.dtype))
         y = product(*quantize(h), self.down, offsets, self.hidden, x.dtype)
-        # a padding token's slots are -1 and its gates 0: any row will do
-        picked = y[slot.clamp(min=0).reshape(-1).long()].view(tokens, self.topk, self.width)
+        # where some slot is -1 there are fewer ordered rows than slots, and the last row, which -1 names, is in no group: zeros
+        picked = y[slot.reshape(-1).long()].view(tokens, self.topk, self.width)
         return torch.einsum("tkw,tk->tw", picked.float(), gate).to(x.dtype), idx
 
 

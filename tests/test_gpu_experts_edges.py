@@ -337,3 +337,17 @@ def test_strided_vectors_and_packed_matrices():
             rows = slice(int(off[2 * g]), int(off[2 * g + 2]))
             assert torch.equal(one[rows], plain[rows])
             assert torch.equal(experts.product(xq[rows][:1], xs[rows][:1], (wq[g:g + 1], ws[g:g + 1]), None, 96, torch.float32), plain[rows][:1])
+
+
+def test_layer_padding_stays_zero_when_an_expert_overflows():
+    """The first row of the ordered products belongs to some token; what it holds reaches that token alone."""
+    import torch
+    from paper_2502_07021_b200 import experts
+    layer, x = make_layer(2, k=2, dtype="float16"), tokens_of(5, dtype="float16")
+    layer.up = experts.quantize(torch.full((2, 96, 64), 3.0, dtype=torch.float16, device="cuda"))
+    x[0] = 1000.0                                      # 64 x 3000 is beyond fp16
+    x[1:] = 1.0
+    mask = torch.tensor([1, 1, 0, 1, 0], dtype=torch.uint8, device="cuda")
+    y, _ = layer(x, mask)
+    got = host(y)
+    assert not np.any(np.isfinite(got[0])) and np.all(got[[2, 4]] == 0) and np.all(np.isfinite(got[[1, 3]]))
