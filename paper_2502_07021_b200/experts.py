@@ -180,7 +180,9 @@ class RoutedExperts:
         tokens, experts = x.shape[0], self.score.shape[0]
         stream = torch.cuda.current_stream(x.device)
         logits = x @ self.score.T
-        _, bias, _ = balance(logits, self.eps, self.iters, mask)
+        # a token whose scores are no numbers would make every dual NaN: it takes no part, and its gates are NaN
+        sound = logits.amax(1) < float("inf")
+        _, bias, _ = balance(logits, self.eps, self.iters, sound if mask is None else sound & (mask != 0))
         idx, gate = choose(logits, self.topk, bias, mask)
         pairs = tokens * self.topk
         work, size = _scratch(tokens, experts, self.topk, x.device)

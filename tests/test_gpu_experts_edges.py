@@ -351,3 +351,19 @@ def test_layer_padding_stays_zero_when_an_expert_overflows():
     y, _ = layer(x, mask)
     got = host(y)
     assert not np.any(np.isfinite(got[0])) and np.all(got[[2, 4]] == 0) and np.all(np.isfinite(got[[1, 3]]))
+
+
+def test_layer_with_a_token_of_nan():
+    """One such token costs itself and nobody else."""
+    import torch
+    layer, x = make_layer(12, k=3), tokens_of(200)
+    mask = torch.ones(200, dtype=torch.bool, device="cuda")
+    mask[50] = False
+    want, want_idx = layer(x, mask)                    # the batch without the token
+    x[50, 7] = float("nan")
+    y, idx = layer(x)
+    rest = np.arange(200) != 50
+    assert np.all(np.isnan(host(y)[50])) and np.all(idx.cpu().numpy()[50] == -1)
+    assert torch.equal(idx[mask], want_idx[mask]) and np.array_equal(host(y)[rest], host(want)[rest])
+    y, idx = layer(x, mask)                            # as padding it counts for nothing
+    assert torch.equal(idx, want_idx) and torch.equal(y, want)
