@@ -4,7 +4,8 @@
 
 ``RoutedExperts`` is the serving form: tokens are scored, balanced against the experts' shares by Sinkhorn iterations (the
 duals are added to the scores for the choice only), ordered by expert, rounded to 4 bits once each, and sent through their
-experts' 4-bit matrices.  ``route`` is the training form of the router alone: a differentiable function of the scores whose
+experts' 4-bit matrices.  A prompt is balanced by itself; a decode step takes the duals that were kept from a batch
+(``layer.duals``), since a few tokens say nothing about the experts' load.  ``route`` is the training form of the router alone: a differentiable function of the scores whose
 backward pass is ``fs_router_backward``.
 
 Everything runs on the current stream of the tensors' device; the balance, choice, ordering and products are the library's
@@ -172,17 +173,41 @@ class RoutedExperts:
         self.width, self.hidden = width, hidden
         self.up, self.down = quantize(up), quantize(down)   # laid out once
 
-    def __call__(self, x, mask=None):
+    def duals(self, x, mask=None):
+        """Duals [experts] of a batch's balance, to be kept and handed to later calls as their bias.
+
+        Fewer tokens than experts are not balanced, the duals are then 0: with a share of less than one token per expert the
+        balance spreads every token over several experts whatever its scores are; one token alone ends up indifferent."""
+        x, mask = self._batch(x, mask)
+        return self._duals(x @ self.score.T, mask)
+
+    def _batch(self, x, mask):
         if x.dim() != 2 or x.shape[1] != self.width:
             raise ValueError("x: [tokens, width]")
         _together(x.device, score=self.score)
         x = _rows(x)
+        return x, _mask(mask, x)
+
+    def _duals(self, logits, mask):
+        tokens, experts = logits.shape
+        if tokens < experts:
+            return torch.zeros(experts, device=logits.device)
+        # a token whose scores are no numbers would make every dual NaN: it takes no part, and its gates are NaN
+        sound = logits.amax(1) < float("inf")
+        if mask is not None:
+            sound &= mask != 0
+        g = balance(logits, self.eps, self.iters, sound)[1]
+        return torch.where(sound.sum() >= experts, g, 0.0)
+
+    def __call__(self, x, mask=None, bias=None):
+        """(y [tokens, width], idx [tokens, topk]).  mask: 0 for padding.  bias: duals [experts] for the choice, kept from an
+        earlier batch (``duals``); None for those of this batch."""
+        x, mask = self._batch(x, mask)
         tokens, experts = x.shape[0], self.score.shape[0]
         stream = torch.cuda.current_stream(x.device)
         logits = x @ self.score.T
-        # a token whose scores are no numbers would make every dual NaN: it takes no part, and its gates are NaN
-        sound = logits.amax(1) < float("inf")
-        _, bias, _ = balance(logits, self.eps, self.iters, sound if mask is None else sound & (mask != 0))
+        if bias is None:
+            bias = self._duals(logits, mask)
         idx, gate = choose(logits, self.topk, bias, mask)
         pairs = tokens * self.topk
         work, size = _scratch(tokens, experts, self.topk, x.device)
@@ -218,6 +243,8 @@ def main():
               f"gradient norm {leaf.grad.norm():.3e}")
     y, _ = layer(x)
     print(f"layer output {tuple(y.shape)} {y.dtype}, rms {y.float().pow(2).mean().sqrt():.3f}")
+    y, idx = layer(x[:1], bias=layer.duals(x))         # a decode step with the batch's duals
+    print(f"one token: experts {idx[0].tolist()}, rms {y.float().pow(2).mean().sqrt():.3f}")
 
 
 if __name__ == "__main__":

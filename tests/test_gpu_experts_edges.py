@@ -367,3 +367,40 @@ def test_layer_with_a_token_of_nan():
     assert torch.equal(idx[mask], want_idx[mask]) and np.array_equal(host(y)[rest], host(want)[rest])
     y, idx = layer(x, mask)                            # as padding it counts for nothing
     assert torch.equal(idx, want_idx) and torch.equal(y, want)
+
+
+@pytest.mark.parametrize("tokens", [1, 2, 31, 63])
+def test_layer_on_few_tokens_chooses_by_the_tokens_scores(tokens):
+    """Fewer tokens than experts cannot be balanced among themselves: every expert's share is less than a token.  The choice is the
+    token's own, or that of the duals kept from a batch."""
+    layer, x = make_layer(64, k=8), tokens_of(tokens)
+    logits = (x @ layer.score.T).float().cpu().numpy()
+    y, idx = layer(x)
+    assert np.array_equal(idx.cpu().numpy(), ref.select(logits, None, None, 8))
+    kept = layer.duals(tokens_of(2000, seed=5))
+    assert np.all(np.isfinite(host(kept))) and np.abs(host(kept)).max() > 0.05
+    y2, idx2 = layer(x, bias=kept)
+    assert np.array_equal(idx2.cpu().numpy(), ref.select(logits, None, kept.cpu().numpy(), 8))
+    assert np.all(np.isfinite(host(y))) and np.all(np.isfinite(host(y2)))
+
+
+def test_layer_on_a_batch_of_mostly_padding():
+    import torch
+    layer, x = make_layer(64, k=8), tokens_of(300)
+    mask = torch.zeros(300, dtype=torch.uint8, device="cuda")
+    mask[40:100] = 2                                   # 60 tokens for 64 experts; any byte but 0 is a token
+    y, idx = layer(x, mask)
+    logits = (x @ layer.score.T).float().cpu().numpy()
+    assert np.array_equal(idx.cpu().numpy(), ref.select(logits, mask.cpu().numpy(), None, 8))
+    off = mask.cpu().numpy() == 0
+    assert np.all(host(y)[off] == 0)
+
+
+def test_layer_with_nan_duals_returns_nan():
+    import torch
+    layer, x = make_layer(12, k=3), tokens_of(30)
+    mask = torch.ones(30, dtype=torch.bool, device="cuda")
+    mask[4] = False
+    y, _ = layer(x, mask, bias=torch.full((12,), float("nan"), device="cuda"))
+    on = mask.cpu().numpy()
+    assert np.all(np.isnan(host(y)[on])) and np.all(host(y)[~on] == 0)
