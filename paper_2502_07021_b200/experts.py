@@ -18,6 +18,14 @@ import torch
 from . import binding as fs
 
 
+def _launch(device, call, *args):
+    """The call on the device's current stream, with the device selected: a launch goes to the current device."""
+    if torch.cuda.current_device() == device.index:
+        return call(*args, torch.cuda.current_stream(device))
+    with torch.cuda.device(device):
+        call(*args, torch.cuda.current_stream(device))
+
+
 def _scratch(tokens, experts, topk, device):
     size = fs.fs_router_workspace(tokens, experts, topk)
     if size == 0:
@@ -80,9 +88,8 @@ def balance(logits, eps, iters, mask=None, share=None, start=None):
     tokens, experts, dtype = _scores(logits)
     work, size = _scratch(tokens, experts, 1, logits.device)
     f, g, err = (torch.empty(n, device=logits.device) for n in (tokens, experts, iters))
-    fs.fs_router_duals(logits, dtype, logits.stride(0), tokens, experts, _mask(mask, logits), _per_expert(share, "share", logits),
-                       eps, iters, _per_expert(start, "start", logits), f, g, err, work, size,
-                       torch.cuda.current_stream(logits.device))
+    _launch(logits.device, fs.fs_router_duals, logits, dtype, logits.stride(0), tokens, experts, _mask(mask, logits),
+            _per_expert(share, "share", logits), eps, iters, _per_expert(start, "start", logits), f, g, err, work, size)
     return f, g, err
 
 
@@ -92,9 +99,9 @@ def choose(logits, topk, bias=None, mask=None, normalize=True):
     work, size = _scratch(tokens, experts, topk, logits.device)
     idx = torch.empty(tokens, topk, dtype=torch.int32, device=logits.device)
     gate = torch.empty(tokens, topk, device=logits.device)
-    fs.fs_router_forward(logits, dtype, logits.stride(0), tokens, experts, _mask(mask, logits), _per_expert(bias, "bias", logits), topk,
-                         fs.FS_ROUTE_NORMALIZE if normalize else 0, idx, gate, None, None, None, None, None, work, size,
-                         torch.cuda.current_stream(logits.device))
+    _launch(logits.device, fs.fs_router_forward, logits, dtype, logits.stride(0), tokens, experts, _mask(mask, logits),
+            _per_expert(bias, "bias", logits), topk, fs.FS_ROUTE_NORMALIZE if normalize else 0, idx, gate, None, None, None, None, None,
+            work, size)
     return idx, gate
 
 
@@ -110,8 +117,8 @@ class _Route(torch.autograd.Function):
         gate, lse = torch.empty(tokens, topk, device=dev), torch.empty(tokens, device=dev)
         load, prob, loss = (torch.empty(n, device=dev) for n in (experts, experts, 2))
         flags = fs.FS_ROUTE_NORMALIZE if normalize else 0
-        fs.fs_router_forward(logits, dtype, logits.stride(0), tokens, experts, mask, bias, topk, flags, idx, gate, lse, counts, load,
-                             prob, loss, work, size, torch.cuda.current_stream(dev))
+        _launch(dev, fs.fs_router_forward, logits, dtype, logits.stride(0), tokens, experts, mask, bias, topk, flags, idx, gate, lse,
+                counts, load, prob, loss, work, size)
         ctx.save_for_backward(logits, idx, gate, lse, counts, load)
         ctx.mask, ctx.flags = mask, flags
         ctx.mark_non_differentiable(idx, counts)
@@ -123,10 +130,9 @@ class _Route(torch.autograd.Function):
         logits, idx, gate, lse, counts, load = ctx.saved_tensors
         tokens, experts, dtype = _scores(logits)
         out = torch.empty(tokens, experts, dtype=logits.dtype, device=logits.device)
-        fs.fs_router_backward(logits, dtype, logits.stride(0), tokens, experts, ctx.mask, idx.shape[1], ctx.flags, idx, gate, lse,
-                              counts, load, None if d_gate is None else d_gate.float().contiguous(),
-                              None if d_loss is None else d_loss.float().contiguous(), out, out.stride(0),
-                              torch.cuda.current_stream(logits.device))
+        _launch(logits.device, fs.fs_router_backward, logits, dtype, logits.stride(0), tokens, experts, ctx.mask, idx.shape[1], ctx.flags,
+                idx, gate, lse, counts, load, None if d_gate is None else d_gate.float().contiguous(),
+                None if d_loss is None else d_loss.float().contiguous(), out, out.stride(0))
         return out, None, None, None, None
 
 
@@ -139,14 +145,15 @@ def quantize(x):
     """(codes, scale bytes) of a matrix or a stack [groups, rows, cols] of them, on the 4-bit microscaled grid."""
     flat = _rows(x.reshape(-1, x.shape[-1]))
     q, s = fs.mx4_empty(flat.shape[0], flat.shape[1], x.device)
-    fs.fs_mx4_quantize(flat, fs.fs_dtype(flat), flat.stride(0), flat.shape[0], flat.shape[1], None, 1, flat.shape[0], q, q.stride(0),
-                       s, s.stride(0), torch.cuda.current_stream(x.device))
+    _launch(x.device, fs.fs_mx4_quantize, flat, fs.fs_dtype(flat), flat.stride(0), flat.shape[0], flat.shape[1], None, 1, flat.shape[0],
+            q, q.stride(0), s, s.stride(0))
     return q.view(*x.shape[:-1], -1), s.view(*x.shape[:-1], -1)
 
 
 def product(xq, xs, weights, offsets, cols, dtype):
-    """Rows ordered by group times their group's 4-bit weights (codes, scales) [groups, outs, ...]; offsets int32 [groups + 1], None for one
-    group of all rows."""
+    """Rows ordered by group times their group's 4-bit weights (codes, scales) [groups, outs, ...].
+
+    offsets: int32 [groups + 1], None for one group of all rows."""
     wq, ws = weights
     rows, groups, outs, nb = xq.shape[0], wq.shape[0], wq.shape[1], -(-cols // 32)
     _together(xq.device, xs=xs, wq=wq, ws=ws, offsets=offsets)
@@ -156,9 +163,13 @@ def product(xq, xs, weights, offsets, cols, dtype):
         offsets = offsets.contiguous()
     pitches = [_packed(t, name, lead, need) for t, name, lead, need in (
         (xq, "xq", (rows,), 16 * nb), (xs, "xs", (rows,), nb), (wq, "wq", (groups, outs), 16 * nb), (ws, "ws", (groups, outs), nb))]
-    y = torch.empty(rows, outs, dtype=dtype, device=xq.device)
-    fs.fs_mx4_product(xq, pitches[0], xs, pitches[1], rows, wq, pitches[2], ws, pitches[3], groups, offsets, outs, cols, y,
-                      fs.fs_dtype(y), y.stride(0), torch.cuda.current_stream(xq.device))
+    return _product(xq, xs, wq, ws, pitches, offsets, outs, cols, dtype)
+
+
+def _product(xq, xs, wq, ws, pitches, offsets, outs, cols, dtype):
+    y = torch.empty(xq.shape[0], outs, dtype=dtype, device=xq.device)
+    _launch(xq.device, fs.fs_mx4_product, xq, pitches[0], xs, pitches[1], xq.shape[0], wq, pitches[2], ws, pitches[3], wq.shape[0], offsets,
+            outs, cols, y, fs.fs_dtype(y), y.stride(0))
     return y
 
 
@@ -169,9 +180,15 @@ class RoutedExperts:
         experts, hidden, width = up.shape
         if score.shape != (experts, width) or down.shape != (experts, width, hidden):
             raise ValueError("score [experts, width], up [experts, hidden, width], down [experts, width, hidden]")
+        _together(score.device, up=up, down=down)
         self.score, self.topk, self.eps, self.iters = score, topk, eps, iters
         self.width, self.hidden = width, hidden
         self.up, self.down = quantize(up), quantize(down)   # laid out once
+
+    @staticmethod
+    def _times(xq, xs, weights, offsets, outs, cols, dtype):
+        packed = (xq, xs, *weights)                     # all of them made by quantize: dense rows
+        return _product(*packed, [t.shape[-1] for t in packed], offsets, outs, cols, dtype)
 
     def duals(self, x, mask=None):
         """Duals [experts] of a batch's balance, to be kept and handed to later calls as their bias.
@@ -194,8 +211,9 @@ class RoutedExperts:
             return torch.zeros(experts, device=logits.device)
         # a token whose scores are no numbers would make every dual NaN: it takes no part, and its gates are NaN
         sound = logits.amax(1) < float("inf")
-        if mask is not None:
-            sound &= mask != 0
+        if mask is None:
+            return balance(logits, self.eps, self.iters, sound)[1]
+        sound &= mask != 0
         g = balance(logits, self.eps, self.iters, sound)[1]
         return torch.where(sound.sum() >= experts, g, 0.0)
 
@@ -204,7 +222,6 @@ class RoutedExperts:
         earlier batch (``duals``); None for those of this batch."""
         x, mask = self._batch(x, mask)
         tokens, experts = x.shape[0], self.score.shape[0]
-        stream = torch.cuda.current_stream(x.device)
         logits = x @ self.score.T
         if bias is None:
             bias = self._duals(logits, mask)
@@ -213,14 +230,14 @@ class RoutedExperts:
         work, size = _scratch(tokens, experts, self.topk, x.device)
         i32 = dict(dtype=torch.int32, device=x.device)
         offsets, rows, slot = torch.empty(experts + 1, **i32), torch.empty(pairs, **i32), torch.empty(tokens, self.topk, **i32)
-        fs.fs_router_dispatch(idx, tokens, self.topk, experts, offsets, rows, slot, work, size, stream)
+        _launch(x.device, fs.fs_router_dispatch, idx, tokens, self.topk, experts, offsets, rows, slot, work, size)
         xq, xs = fs.mx4_empty(pairs, self.width, x.device)
-        fs.fs_mx4_quantize(x, fs.fs_dtype(x), x.stride(0), tokens, self.width, slot, self.topk, pairs, xq, xq.stride(0), xs,
-                           xs.stride(0), stream)
-        h = torch.nn.functional.silu(product(xq, xs, self.up, offsets, self.width, x.dtype))
-        y = product(*quantize(h), self.down, offsets, self.hidden, x.dtype)
+        _launch(x.device, fs.fs_mx4_quantize, x, fs.fs_dtype(x), x.stride(0), tokens, self.width, slot, self.topk, pairs, xq,
+                xq.stride(0), xs, xs.stride(0))
+        h = torch.nn.functional.silu(self._times(xq, xs, self.up, offsets, self.hidden, self.width, x.dtype))
+        y = self._times(*quantize(h), self.down, offsets, self.width, self.hidden, x.dtype)
         # where some slot is -1 there are fewer ordered rows than slots, and the last row, which -1 names, is in no group: zeros
-        picked = y[slot.reshape(-1).long()].view(tokens, self.topk, self.width)
+        picked = y[slot.view(-1)].view(tokens, self.topk, self.width)
         return torch.einsum("tkw,tk->tw", picked.float(), gate).to(x.dtype), idx
 
 
