@@ -294,7 +294,7 @@ extern "C" int fs_mx4_quantize(const void *x_dev, int dtype, int64_t ld, int64_t
     using namespace fsr;
     if (dtype != FS_F32 && dtype != FS_BF16 && dtype != FS_F16) return FS_ERR_BAD_N;
     if (int rc = check_packed(q_out, q_pitch, s_out, s_pitch, rows, cols)) return rc;
-    if ((src_rows > 1 && ld < cols) || src_rows < 0 || copies < 1 || (!slot_dev && (copies != 1 || rows < src_rows))) return FS_ERR_BAD_N;
+    if ((src_rows > 1 && ld < cols) || src_rows < 0 || copies < 1 || (!slot_dev && src_rows > 0 && (copies != 1 || rows < src_rows))) return FS_ERR_BAD_N;
     if (rows == 0 || src_rows == 0) return FS_OK;
     if (!x_dev) return FS_ERR_NULL;
     if (reinterpret_cast<uintptr_t>(x_dev) % type_size(dtype)) return FS_ERR_UNSUPPORTED;

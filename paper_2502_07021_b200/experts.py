@@ -147,7 +147,7 @@ def quantize(x):
     q, s = fs.mx4_empty(flat.shape[0], flat.shape[1], x.device)
     _launch(x.device, fs.fs_mx4_quantize, flat, fs.fs_dtype(flat), flat.stride(0), flat.shape[0], flat.shape[1], None, 1, flat.shape[0],
             q, q.stride(0), s, s.stride(0))
-    return q.view(*x.shape[:-1], -1), s.view(*x.shape[:-1], -1)
+    return q.view(*x.shape[:-1], q.shape[1]), s.view(*x.shape[:-1], s.shape[1])
 
 
 def product(xq, xs, weights, offsets, cols, dtype):

@@ -18,6 +18,13 @@ def test_balance_refuses_an_eps_beyond_fp32(eps):
     assert fs.lib().fs_router_duals(P, fs.FS_F32, 4, 10, 4, None, None, eps, 1, None, None, P, None, P, need, None) == fs.FS_ERR_BAD_EPS
 
 
+def test_rounding_no_rows_to_slots():
+    """An empty array of slots has no address."""
+    lib = fs.lib()
+    assert lib.fs_mx4_quantize(None, fs.FS_BF16, 64, 0, 64, None, 3, 0, None, 32, None, 4, None) == fs.FS_OK
+    assert lib.fs_mx4_quantize(P, fs.FS_BF16, 64, 1, 64, None, 3, 3, P, 32, P, 4, None) == fs.FS_ERR_BAD_N
+
+
 class OnDevice:
     """A CPU tensor that says it lies on another device."""
 

@@ -404,3 +404,17 @@ def test_layer_with_nan_duals_returns_nan():
     y, _ = layer(x, mask, bias=torch.full((12,), float("nan"), device="cuda"))
     on = mask.cpu().numpy()
     assert np.all(np.isnan(host(y)[on])) and np.all(host(y)[~on] == 0)
+
+
+def test_no_tokens_at_all():
+    import torch
+    from paper_2502_07021_b200 import experts
+    layer = make_layer(12, k=3)
+    y, idx = layer(tokens_of(0))
+    assert y.shape == (0, 64) and idx.shape == (0, 3) and torch.all(layer.duals(tokens_of(0)) == 0)
+    l = torch.empty(0, 12, device="cuda", requires_grad=True)
+    gate, loss, idx, counts = experts.route(l, 3)
+    loss.sum().backward()
+    assert l.grad.shape == (0, 12) and torch.all(loss == 0) and torch.all(counts == 0)
+    f, g, err = experts.balance(l.detach(), 0.1, 2)
+    assert f.shape == (0,) and torch.all(g == 0) and torch.all(err == 0)
