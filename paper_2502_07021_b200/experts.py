@@ -119,25 +119,26 @@ class _Route(torch.autograd.Function):
         flags = fs.FS_ROUTE_NORMALIZE if normalize else 0
         _launch(dev, fs.fs_router_forward, logits, dtype, logits.stride(0), tokens, experts, mask, bias, topk, flags, idx, gate, lse,
                 counts, load, prob, loss, work, size)
-        ctx.save_for_backward(logits, idx, gate, lse, counts, load)
-        ctx.mask, ctx.flags = mask, flags
+        ctx.save_for_backward(logits, idx, gate, lse, counts, load, mask)   # a mask changed in place is noticed
+        ctx.flags = flags
         ctx.mark_non_differentiable(idx, counts)
         ctx.set_materialize_grads(False)
         return gate, loss, idx, counts
 
     @staticmethod
+    @torch.autograd.function.once_differentiable
     def backward(ctx, d_gate, d_loss, _idx, _counts):
-        logits, idx, gate, lse, counts, load = ctx.saved_tensors
+        logits, idx, gate, lse, counts, load, mask = ctx.saved_tensors
         tokens, experts, dtype = _scores(logits)
         out = torch.empty(tokens, experts, dtype=logits.dtype, device=logits.device)
-        _launch(logits.device, fs.fs_router_backward, logits, dtype, logits.stride(0), tokens, experts, ctx.mask, idx.shape[1], ctx.flags,
+        _launch(logits.device, fs.fs_router_backward, logits, dtype, logits.stride(0), tokens, experts, mask, idx.shape[1], ctx.flags,
                 idx, gate, lse, counts, load, None if d_gate is None else d_gate.float().contiguous(),
                 None if d_loss is None else d_loss.float().contiguous(), out, out.stride(0))
         return out, None, None, None, None
 
 
 def route(logits, topk, bias=None, mask=None, normalize=True):
-    """Training form: (gate, loss, idx, counts); gate and loss = (balance, mean squared logsumexp) carry gradients."""
+    """Training form: (gate, loss, idx, counts); gate and loss = (balance, mean squared logsumexp) carry first derivatives."""
     return _Route.apply(logits, topk, bias, mask, normalize)
 
 

@@ -418,3 +418,24 @@ def test_no_tokens_at_all():
     assert l.grad.shape == (0, 12) and torch.all(loss == 0) and torch.all(counts == 0)
     f, g, err = experts.balance(l.detach(), 0.1, 2)
     assert f.shape == (0,) and torch.all(g == 0) and torch.all(err == 0)
+
+
+def test_second_derivatives_and_changed_masks_are_refused():
+    import torch
+    from paper_2502_07021_b200 import experts
+    l = torch.randn(20, 8, device="cuda", requires_grad=True)
+    gate, loss, _, _ = experts.route(l, 2)
+    first, = torch.autograd.grad(gate.square().sum() + loss.sum(), l, create_graph=True)
+    with pytest.raises(RuntimeError):
+        first.square().sum().backward()
+    for mask in (torch.ones(20, dtype=torch.bool, device="cuda"), torch.ones(20, dtype=torch.uint8, device="cuda")):
+        gate, loss, _, _ = experts.route(l, 2, mask=mask)
+        loss.sum().backward(retain_graph=True)         # unchanged: twice gives the same
+        one = l.grad.clone()
+        l.grad = None
+        loss.sum().backward(retain_graph=True)
+        assert torch.equal(one, l.grad)
+        mask[3] = 0
+        with pytest.raises(RuntimeError):
+            loss.sum().backward()
+        l.grad = None
