@@ -4,7 +4,8 @@
 // eight, two shuffles for the block's maximum, the scale exponent from the maximum's exponent bits, eight exact products with a
 // power of two, four conversions (cvt.rn.satfinite.e2m1x2), one 4-byte store.  Both directions are bound by HBM: what
 // they move is the matrix once and its 17/32-byte-per-entry packed form once.
-// 16384 x 8192 bf16: 58 us to 4 bits and 57 us back, 340 MB each way, 5.9 TB/s (0.91 of the copy rate).  One span per warp at a time:
+// 16384 x 8192 bf16: 58 - 60 us to 4 bits and as much back, 340 MB each way, 5.7 - 5.9 TB/s (0.88 - 0.91 of the copy rate).  Rows on
+// odd addresses go element by element: 109 and 350 us with a pitch of 8193.  One span per warp at a time:
 // 116 and 75 us; four spans with fp32 arithmetic throughout: 89 and 82, 66 % of the issue slots busy -- hence the packed 16-bit maxima
 // and products, and the decoding by byte permutes.
 #include "router_common.cuh"

@@ -17,10 +17,11 @@
 //   warps 10-17 tcgen05.ld of a finished accumulator (two of them, so this overlaps the next tile), rounding, stores
 // Every wait is bounded; if one runs out the CTA's remaining outputs become NaN and it leaves.
 //
-// Bound and measured.  32768 rows in 32 groups, 4096 x 4096: 313 us, 3.5 PFLOP/s (0.53 of four times the bf16 rate); no single part
-// bounds it: without the operand loads 247, the scales 254, three of four matrix instructions 238, the stores 276.  A ring stage
-// goes round in about 825 cycles, and tensor memory (504 of 512 columns) and shared memory have no room for a sixth.  One row for each
-// of 8 groups, 4096 -> 2048: 8.1 us for 36 MB of weights (4.4 TB/s), where 16-wide tiles keep 10 stages of weights under way.
+// Bound and measured.  32768 rows in 32 groups, 4096 x 4096: 304 - 314 us, 3.5 PFLOP/s (0.53 of four times the bf16 rate); no single
+// part bounds it: without the operand loads 247, the scales 254, three of four matrix instructions 238, the stores 276.  A ring stage
+// goes round in about 780 cycles, and tensor memory (504 of 512 columns) and shared memory have no room for a sixth.  One row for each
+// of 8 groups, 4096 -> 2048, where 16-wide tiles keep 10 stages of weights under way: 10.9 us for 36 MB of weights from HBM (3.3 TB/s,
+// eight sets of groups in turn), 8.1 us when the same 36 MB are still in L2.
 // 192 rows per tile is the widest with two accumulators beside the scales' columns.
 #include <cuda.h>
 

@@ -15,14 +15,15 @@
 // losses.  One block finishes by itself, up to eight form a cluster whose first block reads the others' sums.  Floating sums never meet an atomic; the integer counts do, where
 // order does not matter.
 //
-// Backward.  One sweep per token: p = 2^((l - lse) log2 e), over its sum where lse is large, the gate terms scattered into a per-group row in shared
-// memory (topk stores, cleared again after use), F = sum p load by a group reduction, and
+// Backward.  One sweep per token: p = 2^((l - lse) log2 e), over its sum where lse is large, the gate terms scattered into a per-group
+// row in shared memory (topk stores, cleared again after use), F = sum p load by a group reduction, and
 //      dl = direct + p (S (load - F) + Z - a)
 // with S = d0 E / T', Z = 2 d1 lse / T' and the gate's constants; logits are read once and the gradient written once.
 //
-// Measured at 32768 x 256 bf16, top 8.  Forward 33 us: bound by instruction issue, about 650 warp instructions per token, 400 of
-// them the choice (rounds of an arg max over value and column: 73 us; sorted lists: 51); finishing kernel about 5 of it.
-// Backward 13 us for 33.5 MB (2.5 TB/s), issue again, about 250 instructions per token.  Ordering 131072 pairs of 128 experts: 11 us.
+// Measured at 32768 x 256 bf16, top 8.  Forward 34 us: bound by instruction issue, about 650 warp instructions per token, 400 of
+// them the choice (rounds of an arg max over value and column: 73 us; sorted lists: 51); finishing kernel about 5 of it.  At 64
+// registers, two blocks of 512, the instances for 33 to 256 experts spill 84 to 172 bytes a thread.
+// Backward 13.3 us for 33.5 MB (2.5 TB/s), issue again, about 250 instructions per token.  Ordering 131072 pairs of 128 experts: 11 us.
 #include "router_common.cuh"
 
 namespace fsr {
